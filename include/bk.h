@@ -469,7 +469,7 @@ typedef struct bk_matrix {
  * The tensors of a call must not overlap, O over its own G excepted
  * (BK_ERR_INVALID_VALUE); G may be shared.  The workspace (4 bytes for each
  * element and 4 for each of min(d, p)^2 of the matrices padded to multiples of
- * 64, twice that with BK_NS_F32; little or none for matrices with a side of 64 or
+ * 64, twice that with BK_NS_F32; none to 3 MB for a matrix with a side of 64 or
  * less; at most 36 matrices are worked on at a time) is the same for both calls;
  * it depends on d, p and prec only.  The arrays mats
  * and coef are read during the call only. */

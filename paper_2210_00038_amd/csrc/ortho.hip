@@ -976,18 +976,23 @@ __global__ __launch_bounds__(kSmallThreads) void ns_small_kernel(const NsSmallAr
 }
 
 // ---------------------------------------------------------------------------
-// Thin matrices: m <= 64 rows of X, n of any length.  All steps' polynomials are
-// those of one m x m matrix, A = X X^T / |X|^2, so X is needed twice only: for A,
-// and to be multiplied by the product P of all steps' Bm,
+// Thin matrices: m <= 64 rows of X, n of any length.  The polynomials of several
+// steps (a round) are those of one m x m matrix, A = X X^T / |X|^2, so X is needed
+// twice only: for A, and to be multiplied by the product P of the round's Bm,
 //   per step  Bm = a I + b A + c A^2,  P <- Bm P,  A <- Bm A Bm.
 // The square root of A's rounding error is what small singular values are lost
-// in, and they grow 485-fold: in float32 this form loses them, in float64
-// (2^-53 against 485^-2 = 2^-18) it is as good as float32 products of X itself.
-// Next to 3 launches for each step of the general path: 3 in all, and G and M
-// pass memory twice.  Kernel times: one 16 x 4096 21 us, 24 of them 34, one 48 x
-// 3000 64, one 64 x 3000 108 (of them 60 in the polynomials' one workgroup), 24
-// of them 127; the general path takes 115 for one 65 x 3000 and 172 for 24, in the
-// float32-accurate form 210 and 288.
+// in, and they grow 485-fold in five usual steps: in float32 this form loses
+// them, in float64 (2^-53 against 485^-2 = 2^-18) it is as good as float32
+// products of X itself.  Where further steps would lose that again (the rule is
+// the host's), another round begins with the Gram matrix of P X.  P X is not kept:
+// each launch multiplies the chunk that it has loaded by the P of all rounds so
+// far, which costs the usual one round nothing and many rounds no memory.
+// Next to 3 launches for each step of the general path: 3 in all for one round,
+// two more for each other, and G and M pass memory once a launch over chunks.
+// Kernel times: one 16 x 4096 20 us, 24 of them 32, one 48 x 3000 63, one 64 x 3000
+// 107 (of them 60 in the polynomials' one workgroup; 10 steps 207, 20 steps 429),
+// 24 of them 126; the general path takes 115 for one 65 x 3000 and 172 for 24, in
+// the float32-accurate form 210 and 288.
 // ---------------------------------------------------------------------------
 constexpr int kThinThreads = 256;
 
@@ -1039,10 +1044,25 @@ __device__ __forceinline__ void settle64(f64x4_t& a) {
     asm volatile("s_nop 15\n\ts_nop 7");
     asm volatile("" : "+v"(a));
 }
-// Partial Gram matrix of a chunk's columns: every wave the whole of it over a
-// quarter of the columns, the waves' sums joined in order.
+// What the polynomials' launch leaves behind the partial Grams: 1 / (|U| + eps),
+// and the product P of each round.
+__device__ __forceinline__ const double* thin_inv(const NsThinArgs& args, const NsThinMat& L, int m16) {
+    return args.ws + L.gram + (size_t)L.chunks * m16 * m16;
+}
+// P of a round to LDS (a barrier has to follow).
 template <int MT>
-__device__ __forceinline__ void thin_gram(const NsThinArgs& args, const NsThinMat& L, int chunk, int cols, float* X, double* sum) {
+__device__ __forceinline__ void thin_load_poly(const double* inv, int round, float* P) {
+    constexpr int m16 = 16 * MT;
+    const float* poly = reinterpret_cast<const float*>(inv + 1) + (size_t)round * m16 * m16;
+    for (int e = threadIdx.x; e < m16 * m16; e += kThinThreads) P[e / m16 * (m16 + 4) + e % m16] = poly[e];
+}
+
+// Partial Gram matrix of a chunk's columns: every wave the whole of it over a
+// quarter of the columns, the waves' sums joined in order.  FIRST: of U, whose
+// momentum is brought up to date; else of X after args.round rounds.
+template <int MT, bool FIRST>
+__device__ __forceinline__ void thin_gram(const NsThinArgs& args, const NsThinMat& L, int chunk, int cols, float* X, double* sum,
+                                          float* P) {
     constexpr int m16 = 16 * MT, TILES = MT * (MT + 1) / 2;
     const int n = max(L.t.d, L.t.p), ldx = cols + 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1053,7 +1073,18 @@ __device__ __forceinline__ void thin_gram(const NsThinArgs& args, const NsThinMa
     const int end = min(n, (chunk + 1) * L.cols);
     for (int j0 = chunk * L.cols; j0 < end; j0 += cols) {
         const int here = min(cols, end - j0);
-        thin_load<true>(args, L.t, j0, here, m16, ldx, 1.0, X);
+        if constexpr (FIRST) {
+            thin_load<true>(args, L.t, j0, here, m16, ldx, 1.0, X);
+        } else {
+            const double* inv = thin_inv(args, L, m16);
+            thin_load<false>(args, L.t, j0, here, m16, ldx, inv[0], X);
+            for (int r = 0; r < args.round; ++r) {
+                thin_load_poly<MT>(inv, r, P);
+                __syncthreads();
+                ns_apply_columns<MT, kThinThreads / 64>(X, P, m16 + 4, (here + 15) / 16, ldx);
+                __syncthreads();
+            }
+        }
         for (int k = 4 * wave; k < here; k += 16) {          // what follows the columns is zero
             double x[MT];
 #pragma unroll
@@ -1095,16 +1126,18 @@ __device__ __forceinline__ int thin_chunk(const NsThinArgs& args, int& chunk) {
     return find_matrix(args.n, blockIdx.x, chunk, [&](int k) { return args.L[k].begin; });
 }
 
+template <bool FIRST>
 __global__ __launch_bounds__(kThinThreads) void ns_thin_gram_kernel(const NsThinArgs args) {
     __shared__ __attribute__((aligned(16))) float X[kNsThinFloats + 64 * 4];
     __shared__ double sum[64 * 64];
+    __shared__ __attribute__((aligned(16))) float P[FIRST ? 4 : 64 * 68];
     int chunk;
     const NsThinMat& L = args.L[thin_chunk(args, chunk)];
     switch ((min(L.t.d, L.t.p) + 15) / 16) {
-        case 1: thin_gram<1>(args, L, chunk, kNsThinFloats / 16, X, sum); break;
-        case 2: thin_gram<2>(args, L, chunk, kNsThinFloats / 32, X, sum); break;
-        case 3: thin_gram<3>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, sum); break;
-        default: thin_gram<4>(args, L, chunk, kNsThinFloats / 64, X, sum); break;
+        case 1: thin_gram<1, FIRST>(args, L, chunk, kNsThinFloats / 16, X, sum, P); break;
+        case 2: thin_gram<2, FIRST>(args, L, chunk, kNsThinFloats / 32, X, sum, P); break;
+        case 3: thin_gram<3, FIRST>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, sum, P); break;
+        default: thin_gram<4, FIRST>(args, L, chunk, kNsThinFloats / 64, X, sum, P); break;
     }
 }
 
@@ -1167,28 +1200,30 @@ __device__ __forceinline__ void thin_poly(const NsThinArgs& args, const NsThinMa
         }
     }
     __syncthreads();
-    double sq = 0.0;
-    for (int i = 0; i < m16; ++i) sq += A[i * ld + i];
-    const double inv = 1.0 / (sqrt(sq) + (double)args.eps);
-    __syncthreads();
-    for (int e = threadIdx.x; e < m16 * m16; e += kPolyThreads) {
-        // U's scale is taken out one factor at a time: its square may be out of range
-        const int at = e / m16 * ld + e % m16;
-        A[at] = A[at] * inv * inv;
+    double* out = gram + (size_t)L.chunks * m16 * m16;
+    if (args.round == 0) {
+        double sq = 0.0;
+        for (int i = 0; i < m16; ++i) sq += A[i * ld + i];
+        const double inv = 1.0 / (sqrt(sq) + (double)args.eps);
+        __syncthreads();
+        for (int e = threadIdx.x; e < m16 * m16; e += kPolyThreads) {
+            // U's scale is taken out one factor at a time: its square may be out of range
+            const int at = e / m16 * ld + e % m16;
+            A[at] = A[at] * inv * inv;
+        }
+        if (threadIdx.x == 0) out[0] = inv;
+        __syncthreads();
     }
-    __syncthreads();
-    for (int s = 0; s < args.steps; ++s) {
-        double* to = s == 0 ? P : Bm;
+    for (int s = args.first; s < args.last; ++s) {
+        double* to = s == args.first ? P : Bm;
         thin_product<MT>(A, A, to, true, args.coef[3 * s], args.coef[3 * s + 1], args.coef[3 * s + 2]);
-        if (s + 1 < args.steps) {
+        if (s + 1 < args.last) {
             thin_product<MT>(to, A, A, false, 0.0, 0.0, 0.0);
             thin_product<MT>(to, A, A, false, 0.0, 0.0, 0.0);
         }
-        if (s > 0) thin_product<MT>(Bm, P, P, false, 0.0, 0.0, 0.0);
+        if (s > args.first) thin_product<MT>(Bm, P, P, false, 0.0, 0.0, 0.0);
     }
-    double* out = gram + (size_t)L.chunks * m16 * m16;
-    if (threadIdx.x == 0) out[0] = inv;
-    float* poly = reinterpret_cast<float*>(out + 1);
+    float* poly = reinterpret_cast<float*>(out + 1) + (size_t)args.round * m16 * m16;
     for (int e = threadIdx.x; e < m16 * m16; e += kPolyThreads) poly[e] = (float)P[e / m16 * ld + e % m16];
 }
 
@@ -1203,21 +1238,28 @@ __global__ __launch_bounds__(kPolyThreads) void ns_thin_poly_kernel(const NsThin
     }
 }
 
-template <int MT>
+// ONE: there was one round, whose P stays in LDS.
+template <int MT, bool ONE>
 __device__ __forceinline__ void thin_apply(const NsThinArgs& args, const NsThinMat& L, int chunk, int cols, float* X, float* P) {
     constexpr int m16 = 16 * MT, lda = m16 + 4;
     const int n = max(L.t.d, L.t.p), ldx = cols + 4;
-    const double* from = args.ws + L.gram + (size_t)L.chunks * m16 * m16;
-    const double inv = from[0];
-    const float* poly = reinterpret_cast<const float*>(from + 1);
-    for (int e = threadIdx.x; e < m16 * m16; e += kThinThreads) P[e / m16 * lda + e % m16] = poly[e];
+    const double* inv = thin_inv(args, L, m16);
+    const double scale = inv[0];
+    if constexpr (ONE) thin_load_poly<MT>(inv, 0, P);
     const bool tall = L.t.d > L.t.p;
     const int end = min(n, (chunk + 1) * L.cols);
     for (int j0 = chunk * L.cols; j0 < end; j0 += cols) {
         const int here = min(cols, end - j0);
-        thin_load<false>(args, L.t, j0, here, m16, ldx, inv, X);
-        ns_apply_columns<MT, kThinThreads / 64>(X, P, lda, (here + 15) / 16, ldx);
-        __syncthreads();
+        thin_load<false>(args, L.t, j0, here, m16, ldx, scale, X);
+        const int rounds = ONE ? 1 : args.rounds;
+        for (int r = 0; r < rounds; ++r) {
+            if constexpr (!ONE) {
+                thin_load_poly<MT>(inv, r, P);
+                __syncthreads();
+            }
+            ns_apply_columns<MT, kThinThreads / 64>(X, P, lda, (here + 15) / 16, ldx);
+            __syncthreads();
+        }
         const int stop = tall ? L.t.p : min(L.t.p, j0 + here);
         thin_runs(L.t, j0, here, [&](int r, int c) {
             float v[4], w[4];
@@ -1239,16 +1281,17 @@ __device__ __forceinline__ void thin_apply(const NsThinArgs& args, const NsThinM
     }
 }
 
+template <bool ONE>
 __global__ __launch_bounds__(kThinThreads) void ns_thin_apply_kernel(const NsThinArgs args) {
     __shared__ __attribute__((aligned(16))) float X[kNsThinFloats + 64 * 4];
     __shared__ __attribute__((aligned(16))) float P[64 * 68];
     int chunk;
     const NsThinMat& L = args.L[thin_chunk(args, chunk)];
     switch ((min(L.t.d, L.t.p) + 15) / 16) {
-        case 1: thin_apply<1>(args, L, chunk, kNsThinFloats / 16, X, P); break;
-        case 2: thin_apply<2>(args, L, chunk, kNsThinFloats / 32, X, P); break;
-        case 3: thin_apply<3>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, P); break;
-        default: thin_apply<4>(args, L, chunk, kNsThinFloats / 64, X, P); break;
+        case 1: thin_apply<1, ONE>(args, L, chunk, kNsThinFloats / 16, X, P); break;
+        case 2: thin_apply<2, ONE>(args, L, chunk, kNsThinFloats / 32, X, P); break;
+        case 3: thin_apply<3, ONE>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, P); break;
+        default: thin_apply<4, ONE>(args, L, chunk, kNsThinFloats / 64, X, P); break;
     }
 }
 
@@ -1256,12 +1299,18 @@ __global__ __launch_bounds__(kThinThreads) void ns_thin_apply_kernel(const NsThi
 
 hipError_t launch_ns_thin(const NsThinArgs& a, int n_wg, hipStream_t s) {
     if (n_wg <= 0) return hipSuccess;
-    hipLaunchKernelGGL(ns_thin_gram_kernel, dim3(n_wg), dim3(kThinThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(ns_thin_poly_kernel, dim3(a.n), dim3(kPolyThreads), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(ns_thin_apply_kernel, dim3(n_wg), dim3(kThinThreads), 0, s, a);
+    NsThinArgs b = a;
+    for (b.round = 0; b.round < b.rounds; ++b.round) {
+        b.first = b.round > 0 ? b.end[b.round - 1] : 0, b.last = b.end[b.round];
+        if (b.round == 0) hipLaunchKernelGGL(ns_thin_gram_kernel<true>, dim3(n_wg), dim3(kThinThreads), 0, s, b);
+        else hipLaunchKernelGGL(ns_thin_gram_kernel<false>, dim3(n_wg), dim3(kThinThreads), 0, s, b);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(ns_thin_poly_kernel, dim3(b.n), dim3(kPolyThreads), 0, s, b);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (b.rounds == 1) hipLaunchKernelGGL(ns_thin_apply_kernel<true>, dim3(n_wg), dim3(kThinThreads), 0, s, b);
+    else hipLaunchKernelGGL(ns_thin_apply_kernel<false>, dim3(n_wg), dim3(kThinThreads), 0, s, b);
     return hipGetLastError();
 }
 

@@ -280,7 +280,30 @@ void ns_runs(const bk::NsNormArgs& a, int64_t total, int32_t bk::NsMat::*begin, 
 
 struct NsStep {
     float a, b, c, sx, sa, sb, sx2;
+    double gain;                  // the largest factor of a singular value
 };
+
+// Rounds of a thin matrix's steps: end[r] is the first step behind round r.  A
+// round's polynomials come from one Gram matrix, and their product P is rounded to
+// float32, so an error of 2^-53 of an eigenvalue grows by gain^2 in each step (an
+// eigenvalue of zero that rounding made negative leaves the polynomials' range
+// when it nears 1: 18 of the usual steps, or 48 of 1.5 x - 0.5 x^3, gave NaN for
+// updates of low rank), and P's rounding is off by 2^-24 of the product of gains,
+// even in directions that have grown to 1 already.  A product of at most 2^9, the
+// five usual steps (3.4445^5 = 485), keeps both as small as float32 products of X
+// keep theirs: 2^-35 and 2^-15 at most.
+constexpr double kNsRoundGain = 512;
+int ns_rounds(const NsStep* plan, int64_t steps, uint8_t* end) {
+    int rounds = 0;
+    double gain = 1;
+    for (int64_t k = 0; k < steps; ++k) {
+        const double g = std::max(plan[k].gain, 1.0);
+        if (k > 0 && gain * g > kNsRoundGain) end[rounds++] = (uint8_t)k, gain = 1;
+        gain *= g;
+    }
+    end[rounds++] = (uint8_t)steps;
+    return rounds;
+}
 
 bk_status run_ns(const char* fn, const bk_matrix* mats, int64_t n, int prec, bool step, float lr, float beta,
                  bool nesterov, float weight_decay, int64_t steps, const float* coef, float eps, void* ws,
@@ -298,7 +321,8 @@ bk_status run_ns(const char* fn, const bk_matrix* mats, int64_t n, int prec, boo
         const NsBound nb = ns_bound(c[0], c[1], c[2], bound);
         if (!(nb.next <= 64) || !(nb.poly <= 4096))
             return host_fail(BK_ERR_INVALID_VALUE, "%s: the polynomial of step %lld leaves [0, 64]", fn, (long long)k);
-        plan[k] = {c[0], c[1], c[2], ns_scale(bound), ns_scale(bound * bound), ns_scale(nb.poly), ns_scale(nb.next)};
+        plan[k] = {c[0], c[1], c[2], ns_scale(bound), ns_scale(bound * bound), ns_scale(nb.poly), ns_scale(nb.next),
+                   nb.poly};
         bound = nb.next;
     }
     std::vector<Range> used;
@@ -357,7 +381,7 @@ bk_status run_ns(const char* fn, const bk_matrix* mats, int64_t n, int prec, boo
 
     // Thin ones.
     bk::NsThinArgs ta{};
-    ta.steps = (int32_t)steps, ta.nesterov = nesterov, ta.beta = beta, ta.keep = keep, ta.eps = eps;
+    ta.rounds = ns_rounds(plan, steps, ta.end), ta.nesterov = nesterov, ta.beta = beta, ta.keep = keep, ta.eps = eps;
     std::copy(sa.coef, sa.coef + 3 * steps, ta.coef);
     ta.ws = static_cast<double*>(ws);
     int64_t wgs = 0, doubles = 0;

@@ -158,7 +158,8 @@ inline bool ns_is_small(int64_t m, int64_t n) {
     return m <= kNsSmallSide && n <= kNsSmallFloats && (m + 15) / 16 * 16 * ns_small_ld(n) <= kNsSmallFloats;
 }
 hipError_t launch_ns_small(const NsSmallArgs& a, hipStream_t s);
-// Thin matrices (m <= 64, n too long for LDS): three launches.
+// Thin matrices (m <= 64, n too long for LDS): rounds of steps, two launches each
+// and one at the end.
 struct NsThinMat {
     NsSmallMat t;
     int32_t chunks;     // workgroups along n, `cols` columns of X each (a multiple of 16)
@@ -166,13 +167,16 @@ struct NsThinMat {
     int32_t begin;      // first workgroup
     int32_t pad;
     int64_t gram;       // doubles from NsThinArgs::ws to the partial Grams [chunks][m16][m16], then 1 / (|U| + eps)
-                        // and the polynomial (float32 [m16][m16])
+                        // and the rounds' polynomials (float32 [rounds][m16][m16])
 };
 constexpr int kMaxNsThin = 30, kNsThinChunks = 64;
 struct NsThinArgs {
-    int32_t n, steps;
+    int32_t n;
+    int32_t rounds;                 // at most one to a step
     int32_t nesterov;
     float beta, keep, eps;
+    int32_t round, first, last;     // a launch's round, its steps first .. last - 1
+    uint8_t end[kNsMaxSteps];       // round r: steps end[r - 1] (0 for the first) .. end[r] - 1
     double* ws;
     float coef[3 * kNsMaxSteps];
     NsThinMat L[kMaxNsThin];
@@ -182,8 +186,9 @@ constexpr int kNsThinFloats = 8192;                     // of X in a workgroup's
 inline int64_t ns_thin_tile(int64_t m) { return kNsThinFloats / ((m + 15) / 16 * 16) / 16 * 16; }   // its columns
 inline int64_t ns_thin_doubles(int64_t m, int64_t chunks) {
     const int64_t e = (m + 15) / 16 * 16 * ((m + 15) / 16 * 16);
-    return chunks * e + 1 + (e + 1) / 2;
+    return chunks * e + 1 + kNsMaxSteps * (e / 2);
 }
+// Every round of `a` (whose round, first and last are not read).
 hipError_t launch_ns_thin(const NsThinArgs& a, int n_wg, hipStream_t s);
 hipError_t launch_ns_norm(const NsNormArgs& a, int n_wg, hipStream_t s);
 hipError_t launch_ns_prep(const NsArgs& a, int n_wg, bool split, hipStream_t s);
