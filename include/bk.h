@@ -444,10 +444,20 @@ bk_status bk_rmsnorm_grad(const void* dy, const void* xhat, const float* rstd, c
  * (BK_ERR_INVALID_VALUE), steps is 1 to 64.
  *
  * prec: BK_NS_F16: products of fp16 numbers, scaled so that none overflows,
- * with float32 sums; O within about 0.2% (0.5% for ill-conditioned U) of the
- * exact polynomial, in the Frobenius norm.  BK_NS_F32: operands as sums of two
- * fp16 numbers, three times the products; within about 3e-6.  Matrices with a
- * side of 64 or less are as accurate in either.
+ * with float32 sums.  BK_NS_F32: operands as sums of two fp16 numbers, three
+ * times the products.  Matrices with a side of 64 or less are computed in
+ * float32 and float64 in either.
+ * How far O is off, in the Frobenius norm and relative to O, after the five
+ * default steps:
+ *   U of full rank (noised gradients): 0.1 to 0.5% with BK_NS_F16, about 3e-6 with
+ *     BK_NS_F32, and as much as 1.5e-8 sqrt(max(d, p)) more for long sums
+ *   U of rank r below min(d, p): up to 0.3 / sqrt(r) with BK_NS_F16 (15% seen at r = 1,
+ *     4% at r = 8), 4e-4 / sqrt(r) with BK_NS_F32 (sides to 8192), 2e-4 / sqrt(r) with a
+ *     side of 64 or less.  The operands' rounding enters the directions that U
+ *     lacks, where each step multiplies it by a, by 485 in five; float32
+ *     products lose as much as BK_NS_F32.
+ * More steps multiply that further, until those directions are as large as U's
+ * own; O stays within the polynomials' range.
  * Matrices may be of any sizes (d, p <= 2^20, d p <= 2^34); empty ones are
  * skipped.  A zero U gives O = 0 (eps > 0); a NaN or infinity in U makes all
  * of O NaN. */

@@ -722,7 +722,9 @@ def _first(mats, n: int) -> torch.Tensor:
 
 def bk_orthogonalize(mats, n: int, prec: int = BK_NS_F16, steps: int = 5, coef=None, eps: float = 1e-7, ws=None,
                      stream=None):
-    """O of every matrix of `mats` (make_matrices): Newton-Schulz steps on G / (||G||_F + eps)."""
+    """O of every matrix of `mats` (make_matrices): Newton-Schulz steps on G / (||G||_F + eps).  BK_NS_F16 leaves
+    0.1 to 0.5% of O for noised gradients, up to 0.3 / sqrt(r) for ones of rank r; BK_NS_F32 is as accurate as float32
+    products."""
     if n == 0:
         return
     t = _first(mats, n)
@@ -734,7 +736,8 @@ def bk_orthogonalize(mats, n: int, prec: int = BK_NS_F16, steps: int = 5, coef=N
 
 def bk_muon_step(mats, n: int, prec: int = BK_NS_F16, lr: float = 1e-3, beta: float = 0.95, nesterov: bool = True,
                  weight_decay: float = 0.0, steps: int = 5, coef=None, eps: float = 1e-7, ws=None, stream=None):
-    """A Muon step on every matrix of `mats` (make_matrices): momentum, orthogonalisation, weights."""
+    """A Muon step on every matrix of `mats` (make_matrices): momentum, orthogonalisation (whose accuracy
+    bk_orthogonalize states), weights."""
     if n == 0:
         return
     t = _first(mats, n)

@@ -129,6 +129,55 @@ def test_usual_coefficients(bk, d, p):
         assert err <= 4 * plain + SUMS * norm, (steps, err / norm, plain / norm)
 
 
+# What the header says of updates of rank r after the five default steps, relative to O, times sqrt(r), and of
+# long sums.  fp16 operands: X and Bm of each step are rounded, by 2e-4 root mean square (half a step is 2^-12 to
+# 2^-11 of a number); each error is multiplied by at most 3.4445^5 = 485 and O has norm sqrt(r):
+# sqrt(10) 485 2e-4 = 0.3.  22-bit operands: 6e-8 in place of 2e-4 is 9e-5; the float32 sum of a
+# product is of up to 3 n / 16 additions, off by 2^-25 0.6 sqrt(3 n / 16) (2.7e-4 after 485 at n = 5120; 3e-4 at 8192).
+# Float32 (side of at most 64): 2.4e-8 is 4e-5, and n / 4 additions 485 2^-25 0.6 sqrt(n / 4), 1.2e-4 at n = 768.
+LOW_RANK = {"f16": 0.3, "f32": 4e-4, "side": 2e-4}
+LONG = 1.5e-8
+
+
+def _exact_steps(G, steps=5):
+    """Steps of the usual coefficients in float64 on the GPU."""
+    X = G.double()
+    X = (X.T if X.shape[0] > X.shape[1] else X).contiguous() / X.norm()
+    a, b, c = so.NS_QUINTIC
+    for _ in range(steps):
+        A = X @ X.T
+        B = b * A + c * (A @ A)
+        B.diagonal().add_(a)
+        X = B @ X
+    return X.T if G.shape[0] > G.shape[1] else X
+
+
+def _error(bk, G, prec):
+    O, want = torch.empty_like(G), _exact_steps(G)
+    bk.bk_orthogonalize(bk.make_matrices([{"G": G, "O": O}]), 1, prec)
+    return ((O.double() - want).norm() / want.norm()).item()
+
+
+@pytest.mark.parametrize("d,p", [(16, 768), (96, 64), (16, 4096), (2000, 64), (200, 300), (768, 768), (1280, 5120), (2999, 201)])
+def test_low_rank_accuracy(bk, d, p):
+    gen = torch.Generator(device=DEV).manual_seed(d + p)
+    for r in (1, 2, 8, 32, 128):
+        if r >= min(d, p):
+            continue
+        G = torch.randn(d, r, generator=gen, device=DEV) @ torch.randn(r, p, generator=gen, device=DEV)
+        for prec, name in ((bk.BK_NS_F16, "f16"), (bk.BK_NS_F32, "f32")):
+            err = _error(bk, G, prec)
+            assert err <= LOW_RANK["side" if min(d, p) <= 64 else name] / r ** 0.5, (r, name, err)
+
+
+def test_long_sums(bk):
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    for n in (4000, 1 << 17, 1 << 20):
+        G = torch.randn(70, n, generator=gen, device=DEV)
+        assert _error(bk, G, bk.BK_NS_F16) <= 5e-3
+        assert _error(bk, G, bk.BK_NS_F32) <= 3e-6 + LONG * n ** 0.5, n
+
+
 def test_muon_step_of_many_steps(bk):
     """Momentum is brought up to date once, however often U is read; a stack equals single calls, a captured
     call its eager one, and nothing behind the workspace is written."""
