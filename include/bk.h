@@ -417,8 +417,9 @@ bk_status bk_private_grad_noalloc(const bk_layer* layers, int64_t n, bk_dtype dt
  * P is the per-sample gradient of gamma (one sample of all rows: its ordinary
  * gradient), summed in a fixed order; a BK_NORM_AFFINE layer flagged
  * BK_LAYER_KEPT takes it as it is.  dres, dx or P may be NULL (dx or P is
- * needed); dx may be dy, xhat or dres itself.  The workspace is needed for P alone
- * and depends on all of B, T and p: ask for each.  T = 0 gives P = 0. */
+ * needed); dx may be dy, xhat or dres itself.  The workspace is needed for P alone;
+ * its size for B samples serves every smaller batch of the same T and p.  T = 0
+ * gives P = 0. */
 bk_status bk_rmsnorm(const void* x, const void* res, const void* gamma, bk_dtype dt,
                      bk_dtype gamma_dt, int64_t rows, int64_t p, float eps, void* h, void* y,
                      void* xhat, float* rstd, void* q, float* q_scale, int64_t q_group,

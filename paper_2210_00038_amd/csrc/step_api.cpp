@@ -83,6 +83,24 @@ size_t rms_grad_ws(int64_t B, int64_t T, int64_t p) {
     const RmsGradPlan g = rms_grad_plan(B, T, p);
     return g.chunks > 1 ? (size_t)B * g.chunks * p * sizeof(float) : 0;
 }
+// At least rms_grad_ws of B and of every smaller batch, where a workgroup takes
+// fewer rows and more partial rows may be needed.  b samples in runs of `most` rows
+// or more: b ceil(T / most) partial rows, and b + 1024 at most, as a run has b T /
+// 1024 rows or more (from 1024 samples on all T).  Runs that are shorter than 16
+// rows have b T / 256 or more: b T, and b + 256 at most, for less than 256 samples.
+size_t rms_grad_ws_bound(int64_t B, int64_t T, int64_t p) {
+    const int64_t R = bk::rms_grad_rows(p), most = cdiv(kRmsGradMinRows, R) * R;
+    int64_t parts = 0;
+    if (T > most) {
+        const int64_t b = std::min(B, kRmsGradGroups - 1);
+        parts = std::min(b * cdiv(T, most), b + kRmsGradGroups);
+    }
+    if (R == 1 && T > 1) {
+        const int64_t b = std::min(B, kRmsGradFewGroups - 1);
+        parts = std::max(parts, std::min(b * T, b + kRmsGradFewGroups));
+    }
+    return (size_t)parts * p * sizeof(float);
+}
 
 // ------------------------------------------------------- orthogonalised updates
 constexpr size_t kAlign = 256;
@@ -517,7 +535,7 @@ bk_status bk_rmsnorm(const void* x, const void* res, const void* gamma, bk_dtype
 
 size_t bk_rmsnorm_grad_workspace_size(int64_t B, int64_t T, int64_t p) {
     if (check_rms("bk_rmsnorm_grad_workspace_size", BK_F32, B, T, p, nullptr, BK_F32) != BK_OK || B * T == 0) return 0;
-    return rms_grad_ws(B, T, p);
+    return rms_grad_ws_bound(B, T, p);
 }
 
 bk_status bk_rmsnorm_grad(const void* dy, const void* xhat, const float* rstd, const void* gamma, const void* dres,
