@@ -480,6 +480,28 @@ def bk_philox_raw(seed: int, tensor_id: int, step: int, q0: int, nq: int, out=No
 
 
 # -------------------------------------------------------------------- grouped
+def _kept(s: dict) -> torch.Tensor:
+    """P of a kept layer, whose sizes are P's alone: the other tensors have to fit them."""
+    if s.get("P") is None or (s.get("bias") and s.get("Pb") is None):
+        raise ValueError("a kept layer needs P, and with a bias Pb")
+    P = _dev(s["P"], "P")
+    if P.dtype != torch.float32 or P.dim() != 2:
+        raise ValueError("P must be float32 [B, p]")
+    for f, n in (("Pb", P.numel()), ("G", P.shape[1]), ("Gb", P.shape[1])) if s.get("bias") else (("G", P.shape[1]),):
+        t = s.get(f)
+        if t is not None and (_dev(t, f).dtype != torch.float32 or t.numel() != n or t.device != P.device):
+            raise ValueError(f"{f} of a kept layer must be float32 of {n} elements on {P.device}")
+    return P
+
+
+def _batch(layers, n: int, B: int) -> int:
+    """B, if the kept ones of the first n layers hold as many samples."""
+    for k, rows in getattr(layers, "_kept_rows", ()):
+        if k < n and rows < B:
+            raise ValueError(f"layer {k}: its P holds {rows} samples, not {B}")
+    return B
+
+
 def make_layers(specs: Sequence[dict]):
     """ctypes bk_layer array from dicts {kind, x, g, G (optional), V (embedding),
     mixopt (optional bool), P (optional float32 [B,d,p], BK-MixOpt store; [B,p] gamma
@@ -493,15 +515,14 @@ def make_layers(specs: Sequence[dict]):
     to the tensors, so they stay allocated while it is in use."""
     arr = (bk_layer * max(1, len(specs)))()
     arr._tensors = [s.get(k) for s in specs for k in ("x", "g", "G", "P", "Gb", "Pb") if s.get(k) is not None]
+    arr._kept_rows = []
     for k, s in enumerate(specs):
         G = s.get("G")
         kind = s.get("kind", BK_LINEAR)
         if s.get("kept"):
-            for f in ("P", "Pb") if s.get("bias") else ("P",):
-                t = _dev(s[f], f)
-                if t.dtype != torch.float32 or t.dim() != 2:
-                    raise ValueError(f"{f} must be float32 [B, p]")
-            arr[k].kind, arr[k].T, arr[k].d, arr[k].p = kind, 0, s["P"].shape[1], s["P"].shape[1]
+            P = _kept(s)
+            arr._kept_rows.append((k, P.shape[0]))
+            arr[k].kind, arr[k].T, arr[k].d, arr[k].p = kind, 0, P.shape[1], P.shape[1]
             arr[k].flags = (BK_LAYER_KEPT | (BK_LAYER_BIAS if s.get("bias") else 0) |
                             (BK_LAYER_ACCUMULATE if s.get("accumulate") else 0))
             arr[k].G, arr[k].P, arr[k].Gb, arr[k].Pb = (_ptr(s.get(f)) for f in ("G", "P", "Gb", "Pb"))
@@ -544,14 +565,14 @@ def bk_private_grad_workspace_size(layers, n: int, dtype: int, B: int) -> int:
 def bk_layer_norms(layers, n: int, dtype: int, B: int, norm_sq, ws=None, device="cuda", stream=None):
     """Norms of every layer (ghost / instantiated by the 2T^2 < pd rule, embedding ghost) -> [n, B]."""
     ws, nws = _workspace(bk_layer_norms_workspace_size(layers, n, dtype, B), device, ws)
-    _check(lib.bk_layer_norms(layers, n, dtype, B, _ptr(norm_sq), _ptr(ws), nws, _stream(stream)),
+    _check(lib.bk_layer_norms(layers, n, dtype, _batch(layers, n, B), _ptr(norm_sq), _ptr(ws), nws, _stream(stream)),
            "bk_layer_norms")
     return norm_sq
 
 
 def bk_weighted_grads(layers, n: int, C, dtype: int, B: int, ws=None, device="cuda", stream=None):
     ws, nws = _workspace(bk_weighted_grads_workspace_size(layers, n, dtype, B), device, ws)
-    _check(lib.bk_weighted_grads(layers, n, _ptr(C), dtype, B, _ptr(ws), nws, _stream(stream)),
+    _check(lib.bk_weighted_grads(layers, n, _ptr(C), dtype, _batch(layers, n, B), _ptr(ws), nws, _stream(stream)),
            "bk_weighted_grads")
 
 
@@ -559,7 +580,7 @@ def bk_private_grad_noalloc(layers, n: int, dtype: int, B: int, mode: int, R: fl
                             noise_std: float, seed: int, step: int, norm_sq, C, total_sq=None, stream=None):
     """bk_private_grad with the library's own per-GPU scratch array instead of
     a workspace (nothing is allocated; calls on one GPU must not overlap)."""
-    _check(lib.bk_private_grad_noalloc(layers, n, dtype, B, mode, R, gamma, noise_std, seed, step,
+    _check(lib.bk_private_grad_noalloc(layers, n, dtype, _batch(layers, n, B), mode, R, gamma, noise_std, seed, step,
                                        _ptr(norm_sq), _ptr(C), _ptr(total_sq), _stream(stream)),
            "bk_private_grad_noalloc")
 
@@ -569,7 +590,7 @@ def bk_private_grad(layers, n: int, dtype: int, B: int, mode: int, R: float, gam
                     device="cuda", stream=None):
     """Algorithm 1 from the per-layer norms to the noise for a whole stack."""
     ws, nws = _workspace(bk_private_grad_workspace_size(layers, n, dtype, B), device, ws)
-    _check(lib.bk_private_grad(layers, n, dtype, B, mode, R, gamma, noise_std, seed, step, _ptr(norm_sq),
+    _check(lib.bk_private_grad(layers, n, dtype, _batch(layers, n, B), mode, R, gamma, noise_std, seed, step, _ptr(norm_sq),
                                _ptr(C), _ptr(total_sq), _ptr(ws), nws, _stream(stream)), "bk_private_grad")
 
 
