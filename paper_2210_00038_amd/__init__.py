@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -595,6 +596,14 @@ def bk_private_grad(layers, n: int, dtype: int, B: int, mode: int, R: float, gam
 
 
 # ---------------------------------------------------------------- before the path
+def _warn_history(fn: str, backward: str) -> None:
+    """For inputs that require grad: the call stands in a model's forward, where autograd would be expected to
+    follow it."""
+    if torch.is_grad_enabled():
+        warnings.warn(f"{fn}: autograd does not follow this call, its outputs carry no history; use {backward} for the "
+                      "gradients, and detached inputs or torch.no_grad() to say so", stacklevel=3)
+
+
 class RMSNorm(NamedTuple):
     """Outputs of bk_rmsnorm; None: not asked for."""
     y: Optional[torch.Tensor]           # gamma * xhat, x's type
@@ -632,8 +641,13 @@ def bk_rmsnorm(x, gamma=None, residual=None, eps: float = 1e-6, keep: bool = Fal
     """RMS norm of x (+ residual) [..., p]: y, with a residual h = x + residual, with `keep` the
     normalised input and 1 / rms for the backward pass, with `q8` (0: a scale for each row; 32, 64, 128:
     for that many columns) y in e4m3 and its scales.  y=False leaves y out.  Outputs may be given; y, h
-    or xhat may be x or the residual itself."""
+    or xhat may be x or the residual itself.
+
+    Autograd does not follow this call: the outputs carry no history, and their gradients go back through
+    bk_rmsnorm_grad.  An x or residual that requires grad while grad mode is on brings a warning."""
     _dev(x, "x")
+    if x.requires_grad or (residual is not None and residual.requires_grad):
+        _warn_history("bk_rmsnorm", "bk_rmsnorm_grad")
     if x.dim() < 1:
         raise ValueError("x must be [..., p]")
     dt, p = _dtype_code(x), x.shape[-1]
@@ -667,7 +681,8 @@ def bk_rmsnorm_grad_workspace_size(B: int, T: int, p: int) -> int:
 
 def bk_rmsnorm_grad(dy, xhat, rstd, gamma=None, dres=None, dx=None, P=None, ws=None, stream=None):
     """(dx, P) of bk_rmsnorm for dy [B, T, p]: dL/dh, dres added, and the per-sample gradients of gamma
-    [B, p] float32.  dx=False or P=False leaves one out; dx may be dy, xhat or dres itself."""
+    [B, p] float32.  dx=False or P=False leaves one out; dx may be dy, xhat or dres itself.  Autograd does
+    not follow this call."""
     _dev(dy, "dy")
     if dy.dim() != 3:
         raise ValueError("dy must be [B, T, p]")
