@@ -996,6 +996,15 @@ __global__ __launch_bounds__(kSmallThreads) void ns_small_kernel(const NsSmallAr
 // the float32-accurate form 210 and 288.
 // ---------------------------------------------------------------------------
 constexpr int kThinThreads = 256;
+constexpr int kThinLds = kNsThinFloats + 64 * 4;      // floats: 16 MT rows of a tile's columns and four more
+
+// Columns of X in LDS at a time, of 16 MT rows.
+template <int MT>
+constexpr int thin_cols() {
+    constexpr int cols = (int)ns_thin_tile(16 * MT);
+    static_assert(cols >= 16 && cols % 16 == 0 && 16 * MT * (cols + 4) <= kThinLds, "a tile in LDS");
+    return cols;
+}
 
 // f(r, c) for runs of four columns (of a row of U) that cover columns j0 ..
 // j0 + cols of X, one run to a thread and turn: U's columns, or, tall, its rows.
@@ -1062,10 +1071,10 @@ __device__ __forceinline__ void thin_load_poly(const double* inv, int round, flo
 // quarter of the columns, the waves' sums joined in order.  FIRST: of U, whose
 // momentum is brought up to date; else of X after args.round rounds.
 template <int MT, bool FIRST>
-__device__ __forceinline__ void thin_gram(const NsThinArgs& args, const NsThinMat& L, int chunk, int cols, float* X, double* sum,
+__device__ __forceinline__ void thin_gram(const NsThinArgs& args, const NsThinMat& L, int chunk, float* X, double* sum,
                                           float* P) {
-    constexpr int m16 = 16 * MT, TILES = MT * (MT + 1) / 2;
-    const int n = max(L.t.d, L.t.p), ldx = cols + 4;
+    constexpr int m16 = 16 * MT, TILES = MT * (MT + 1) / 2, cols = thin_cols<MT>(), ldx = cols + 4;
+    const int n = max(L.t.d, L.t.p);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, q = lane >> 4;
     f64x4_t acc[TILES];
@@ -1129,16 +1138,16 @@ __device__ __forceinline__ int thin_chunk(const NsThinArgs& args, int& chunk) {
 
 template <bool FIRST>
 __global__ __launch_bounds__(kThinThreads) void ns_thin_gram_kernel(const NsThinArgs args) {
-    __shared__ __attribute__((aligned(16))) float X[kNsThinFloats + 64 * 4];
+    __shared__ __attribute__((aligned(16))) float X[kThinLds];
     __shared__ double sum[64 * 64];
     __shared__ __attribute__((aligned(16))) float P[FIRST ? 4 : 64 * 68];
     int chunk;
     const NsThinMat& L = args.L[thin_chunk(args, chunk)];
     switch ((min(L.t.d, L.t.p) + 15) / 16) {
-        case 1: thin_gram<1, FIRST>(args, L, chunk, kNsThinFloats / 16, X, sum, P); break;
-        case 2: thin_gram<2, FIRST>(args, L, chunk, kNsThinFloats / 32, X, sum, P); break;
-        case 3: thin_gram<3, FIRST>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, sum, P); break;
-        default: thin_gram<4, FIRST>(args, L, chunk, kNsThinFloats / 64, X, sum, P); break;
+        case 1: thin_gram<1, FIRST>(args, L, chunk, X, sum, P); break;
+        case 2: thin_gram<2, FIRST>(args, L, chunk, X, sum, P); break;
+        case 3: thin_gram<3, FIRST>(args, L, chunk, X, sum, P); break;
+        default: thin_gram<4, FIRST>(args, L, chunk, X, sum, P); break;
     }
 }
 
@@ -1241,9 +1250,9 @@ __global__ __launch_bounds__(kPolyThreads) void ns_thin_poly_kernel(const NsThin
 
 // ONE: there was one round, whose P stays in LDS.
 template <int MT, bool ONE>
-__device__ __forceinline__ void thin_apply(const NsThinArgs& args, const NsThinMat& L, int chunk, int cols, float* X, float* P) {
-    constexpr int m16 = 16 * MT, lda = m16 + 4;
-    const int n = max(L.t.d, L.t.p), ldx = cols + 4;
+__device__ __forceinline__ void thin_apply(const NsThinArgs& args, const NsThinMat& L, int chunk, float* X, float* P) {
+    constexpr int m16 = 16 * MT, lda = m16 + 4, cols = thin_cols<MT>(), ldx = cols + 4;
+    const int n = max(L.t.d, L.t.p);
     const double* inv = thin_inv(args, L, m16);
     const double scale = inv[0];
     if constexpr (ONE) thin_load_poly<MT>(inv, 0, P);
@@ -1284,15 +1293,15 @@ __device__ __forceinline__ void thin_apply(const NsThinArgs& args, const NsThinM
 
 template <bool ONE>
 __global__ __launch_bounds__(kThinThreads) void ns_thin_apply_kernel(const NsThinArgs args) {
-    __shared__ __attribute__((aligned(16))) float X[kNsThinFloats + 64 * 4];
+    __shared__ __attribute__((aligned(16))) float X[kThinLds];
     __shared__ __attribute__((aligned(16))) float P[64 * 68];
     int chunk;
     const NsThinMat& L = args.L[thin_chunk(args, chunk)];
     switch ((min(L.t.d, L.t.p) + 15) / 16) {
-        case 1: thin_apply<1, ONE>(args, L, chunk, kNsThinFloats / 16, X, P); break;
-        case 2: thin_apply<2, ONE>(args, L, chunk, kNsThinFloats / 32, X, P); break;
-        case 3: thin_apply<3, ONE>(args, L, chunk, kNsThinFloats / 48 / 16 * 16, X, P); break;
-        default: thin_apply<4, ONE>(args, L, chunk, kNsThinFloats / 64, X, P); break;
+        case 1: thin_apply<1, ONE>(args, L, chunk, X, P); break;
+        case 2: thin_apply<2, ONE>(args, L, chunk, X, P); break;
+        case 3: thin_apply<3, ONE>(args, L, chunk, X, P); break;
+        default: thin_apply<4, ONE>(args, L, chunk, X, P); break;
     }
 }
 

@@ -443,6 +443,7 @@ hipError_t forward(const RmsArgs& a, hipStream_t s) {
 template <typename E, int TPR, int NCH, int BLOCK = block_of<TPR>()>
 hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
     constexpr int rows = BLOCK / TPR;
+    static_assert(rows % rms_rows_at_once(8 * TPR * NCH) == 0, "the host's plan of a sample's rows");
     const int64_t per = a.solo ? rows : 1;
     return in_launches((a.B * a.chunks + per - 1) / per, [&](int64_t at, uint32_t n) {
         RmsGradArgs b = a;
@@ -478,8 +479,6 @@ hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
 }
 
 }  // namespace
-
-int rms_grad_rows(int64_t p) { return p <= 64 ? 32 : p <= 128 ? 16 : p <= 256 ? 8 : p <= 1024 ? 4 : 1; }
 
 hipError_t launch_rmsnorm(const RmsArgs& a, bool bf16, hipStream_t s) {
     return bf16 ? forward<bf16_t>(a, s) : forward<float>(a, s);

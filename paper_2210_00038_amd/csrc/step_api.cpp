@@ -73,7 +73,7 @@ struct RmsGradPlan {
     bool solo;
 };
 RmsGradPlan rms_grad_plan(int64_t B, int64_t T, int64_t p) {
-    const int64_t R = bk::rms_grad_rows(p);
+    const int64_t R = bk::rms_rows_at_once(p);
     if (T < R) return {std::max<int64_t>(T, 1), 1, true};
     const int64_t least = R > 1 ? kRmsGradMinRows : std::min(kRmsGradMinRows, cdiv(B * T, kRmsGradFewGroups));
     const int64_t chunk = cdiv(std::max(least, cdiv(B * T, kRmsGradGroups)), R) * R;
@@ -89,7 +89,7 @@ size_t rms_grad_ws(int64_t B, int64_t T, int64_t p) {
 // 1024 rows or more (from 1024 samples on all T).  Runs that are shorter than 16
 // rows have b T / 256 or more: b T, and b + 256 at most, for less than 256 samples.
 size_t rms_grad_ws_bound(int64_t B, int64_t T, int64_t p) {
-    const int64_t R = bk::rms_grad_rows(p), most = cdiv(kRmsGradMinRows, R) * R;
+    const int64_t R = bk::rms_rows_at_once(p), most = cdiv(kRmsGradMinRows, R) * R;
     int64_t parts = 0;
     if (T > most) {
         const int64_t b = std::min(B, kRmsGradGroups - 1);

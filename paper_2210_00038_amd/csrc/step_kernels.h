@@ -49,9 +49,9 @@ struct RmsGradArgs {
     int32_t chunks;       // ceil(T / chunk)
     int32_t solo;         // each group of threads has a sample of its own
 };
-// Rows a workgroup of the backward kernel works on at once for p columns (more
-// where there are few workgroups).
-int rms_grad_rows(int64_t p);
+// Rows a workgroup of the backward kernel works on at once for p columns (a
+// multiple of that where there are few workgroups).
+constexpr int rms_rows_at_once(int64_t p) { return p <= 64 ? 32 : p <= 128 ? 16 : p <= 256 ? 8 : p <= 1024 ? 4 : 1; }
 hipError_t launch_rmsnorm_grad(const RmsGradArgs& a, bool bf16, hipStream_t s);
 
 // ---- Newton-Schulz orthogonalisation, Muon step -------------------------------
@@ -183,7 +183,7 @@ struct NsThinArgs {
 };
 static_assert(sizeof(NsThinArgs) <= 4096 - 64 && sizeof(NsSmallArgs) <= 4096 - 64, "kernel arguments");
 constexpr int kNsThinFloats = 8192;                     // of X in a workgroup's LDS at a time
-inline int64_t ns_thin_tile(int64_t m) { return kNsThinFloats / ((m + 15) / 16 * 16) / 16 * 16; }   // its columns
+__host__ __device__ constexpr int64_t ns_thin_tile(int64_t m) { return kNsThinFloats / ((m + 15) / 16 * 16) / 16 * 16; }   // its columns
 inline int64_t ns_thin_doubles(int64_t m, int64_t chunks) {
     const int64_t e = (m + 15) / 16 * 16 * ((m + 15) / 16 * 16);
     return chunks * e + 1 + kNsMaxSteps * (e / 2);

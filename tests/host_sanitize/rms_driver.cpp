@@ -30,7 +30,6 @@ hipError_t hipDeviceGetAttribute(int*, hipDeviceAttribute_t, int) { return hipEr
 namespace bk {
 bk_status host_fail(bk_status s, const char*, ...) { return s; }
 bk_status host_hip_fail(hipError_t, const char*) { return BK_ERR_LAUNCH; }
-int rms_grad_rows(int64_t p) { return p <= 64 ? 32 : p <= 128 ? 16 : p <= 256 ? 8 : p <= 1024 ? 4 : 1; }
 hipError_t launch_rmsnorm(const RmsArgs&, bool, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_rmsnorm_grad(const RmsGradArgs& a, bool, hipStream_t) {
     ++launches;

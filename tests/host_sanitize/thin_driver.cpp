@@ -63,7 +63,6 @@ bk_status host_fail(bk_status s, const char* fmt, ...) {
 bk_status host_hip_fail(hipError_t, const char*) { return BK_ERR_LAUNCH; }
 hipError_t launch_rmsnorm(const RmsArgs&, bool, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_rmsnorm_grad(const RmsGradArgs&, bool, hipStream_t) { return hipErrorUnknown; }
-int rms_grad_rows(int64_t) { return 1; }
 hipError_t launch_ns_small(const NsSmallArgs&, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_ns_norm(const NsNormArgs&, int, hipStream_t) { return hipErrorUnknown; }
 hipError_t launch_ns_prep(const NsArgs&, int, bool, hipStream_t) { return hipErrorUnknown; }
