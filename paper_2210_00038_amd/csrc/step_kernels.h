@@ -176,10 +176,10 @@ struct NsThinArgs {
     int32_t nesterov;
     float beta, keep, eps;
     int32_t round, first, last;     // a launch's round, its steps first .. last - 1
-    uint8_t end[kNsMaxSteps];       // round r: steps end[r - 1] (0 for the first) .. end[r] - 1
     double* ws;
     float coef[3 * kNsMaxSteps];
     NsThinMat L[kMaxNsThin];
+    uint8_t end[kNsMaxSteps];       // round r: steps end[r - 1] (0 for the first) .. end[r] - 1 (for the host)
 };
 static_assert(sizeof(NsThinArgs) <= 4096 - 64 && sizeof(NsSmallArgs) <= 4096 - 64, "kernel arguments");
 constexpr int kNsThinFloats = 8192;                     // of X in a workgroup's LDS at a time
