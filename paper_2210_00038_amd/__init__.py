@@ -220,11 +220,18 @@ class _Here:
 _here = _Here()
 
 
+# The current device, and the current stream's handle without a Stream object, whose making takes as long as a
+# call itself: by undocumented functions where this torch has them.
+_device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _on(t: torch.Tensor, stream):
     """The device of t and the stream of a call made current, so that what the call allocates belongs to
     the stream that uses it."""
     if stream is None:
-        return _here if t.get_device() == torch._C._cuda_getDevice() else torch.cuda.device(t.device)
+        return _here if t.get_device() == _device_now() else torch.cuda.device(t.device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, t.device) if stream else torch.cuda.default_stream(t.device)
     if stream.device != t.device:
@@ -233,9 +240,8 @@ def _on(t: torch.Tensor, stream):
 
 
 def _raw_stream(t: torch.Tensor) -> Optional[int]:
-    """Handle of the current stream of t's device (which _on has made current); without a Stream object,
-    whose making takes as long as the call itself."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) or None
+    """Handle of the current stream of t's device (which _on has made current)."""
+    return _raw_stream_of(t.get_device()) or None
 
 
 def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]):
