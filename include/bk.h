@@ -399,7 +399,8 @@ bk_status bk_private_grad_noalloc(const bk_layer* layers, int64_t n, bk_dtype dt
  *   h    = x + res, rounded to dt       (res NULL: h = x)
  *   rstd = 1 / sqrt(mean_j h_j^2 + eps)                     float32 [rows]
  *   xhat = h rstd,  y = gamma * (h rstd)   (gamma [p] of gamma_dt, NULL: ones)
- *   q    = e4m3(y / s), s = max(max |y_j| / 448, 2^-126)    (y before rounding)
+ *   q    = e4m3(y / s), s = max(max |y_j| / 448, 2^-126)    (y before rounding;
+ *          y / s rounded to float32 once, ties to the even code)
  * q [rows, p] holds OCP e4m3 bytes (1.4.3, largest 448), q_scale float32 [rows,
  * ceil(p / q_group)] one s for each q_group columns (32, 64 or 128), or
  * [rows] one for the row (q_group 0).  Sums are float32 and sums of squares

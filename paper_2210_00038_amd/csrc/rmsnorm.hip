@@ -135,31 +135,78 @@ __device__ __forceinline__ void load_gamma(const void* gamma, int bf16, int c, i
     }
 }
 
-// Sum (MAX: maximum) over the TPR threads of a row, the same in all of them.
+// Sum over the TPR threads of a row, the same in all of them.
 // red: TPR / 64 floats; with TPR > 64 the whole workgroup is one row, and red
-// must not be the previous call's, which slower waves may still be reading
-// (callers alternate between two).
-template <int TPR, bool MAX = false>
+// must not be the previous call's, which slower waves may still be reading (the
+// backward pass alternates between two).
+template <int TPR>
 __device__ __forceinline__ float row_reduce(float v, float* red) {
-    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
 #pragma unroll
-    for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1) v = join(v, __shfl_xor(v, off, 64));
+    for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
     if constexpr (TPR > 64) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
         __syncthreads();
         v = red[0];
 #pragma unroll
-        for (int w = 1; w < TPR / 64; ++w) v = join(v, red[w]);
+        for (int w = 1; w < TPR / 64; ++w) v += red[w];
     }
     return v;
 }
 
 template <int TPR> constexpr int block_of() { return TPR > 64 ? TPR : 256; }
 
-template <typename E, int TPR, int NCH>
+// The largest of |y|, and of |h gamma| in float64.
+struct Tops {
+    float y;
+    double t;
+};
+__device__ __forceinline__ Tops larger(Tops a, Tops b) { return {fmaxf(a.y, b.y), fmax(a.t, b.t)}; }
+// Over runs of 4 to 64 lanes, by the vector unit's own paths (by LDS, whose
+// shuffles the groups of a row wait for in turn, [16384, 5120] bf16 in groups of 128
+// took 285 us instead of 262).  The mirrored half (row) of lanes that agree already
+// in fours (eights) serves as the neighbouring one.
+template <typename F>
+__device__ __forceinline__ Tops moved(Tops v, F move) {
+    const uint64_t t = __builtin_bit_cast(uint64_t, v.t);
+    return {__uint_as_float(move(__float_as_uint(v.y))),
+            __builtin_bit_cast(double, (uint64_t)move((uint32_t)(t >> 32)) << 32 | move((uint32_t)t))};
+}
+template <int CTRL>
+__device__ __forceinline__ Tops with_lane(Tops v) {
+    return larger(v, moved(v, [](uint32_t w) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)w, CTRL, 0xF, 0xF, true); }));
+}
+__device__ __forceinline__ Tops run_tops(Tops v, int width) {
+    v = with_lane<0xB1>(v);                     // lane ^ 1
+    v = with_lane<0x4E>(v);                     // lane ^ 2
+    if (width >= 8) v = with_lane<0x141>(v);    // 7 - lane of 8
+    if (width >= 16) v = with_lane<0x140>(v);   // 15 - lane of 16
+    // even rows of 16 (halves) in one result, the odd ones in the other
+    if (width >= 32)
+        v = larger(moved(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[0]; }),
+                   moved(v, [](uint32_t w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false)[1]; }));
+    if (width >= 64)
+        v = larger(moved(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[0]; }),
+                   moved(v, [](uint32_t w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false)[1]; }));
+    return v;
+}
+// Over the TPR threads of a row.
+template <int TPR>
+__device__ __forceinline__ Tops row_tops(Tops v, Tops* wave) {
+    v = run_tops(v, TPR < 64 ? TPR : 64);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = v;
+        __syncthreads();
+        constexpr int waves = TPR / 64, width = waves <= 4 ? 4 : waves <= 8 ? 8 : 16;
+        v = run_tops(wave[min((int)threadIdx.x & (width - 1), waves - 1)], width);
+    }
+    return v;
+}
+
+// Q: 8-bit rows are wanted.
+template <typename E, int TPR, int NCH, bool Q>
 __global__ __launch_bounds__(block_of<TPR>()) void rmsnorm_kernel(const RmsArgs a) {
     constexpr int ROWS = block_of<TPR>() / TPR;
-    __shared__ float red[2][TPR > 64 ? TPR / 64 : 1];
+    __shared__ float red[TPR > 64 ? TPR / 64 : 1];
     const int lane = threadIdx.x % TPR;
     const int p = a.p;
     const int64_t row = a.row0 + (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
@@ -196,83 +243,132 @@ __global__ __launch_bounds__(block_of<TPR>()) void rmsnorm_kernel(const RmsArgs 
     for (int k = 0; k < NCH; ++k)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sq = fmaf(v[k][j], v[k][j], sq);
-    sq = row_reduce<TPR>(sq, red[0]);
+    sq = row_reduce<TPR>(sq, red);
     const float rstd = 1.0f / sqrtf(sq / (float)p + a.eps);
     if (a.rstd && lane == 0) a.rstd[row] = rstd;
+    const auto gamma_of = [&](int k, float w[8]) {
+        if constexpr (EARLY) {
 #pragma unroll
-    for (int k = 0; k < NCH; ++k)
+            for (int j = 0; j < 8; ++j) w[j] = g[k][j];
+        } else {
+            load_gamma(a.gamma, a.gamma_bf16, (k * TPR + lane) * 8, p, w);
+        }
+    };
+    if constexpr (!Q) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] *= rstd;
-    if (a.xhat) {
-        E* o = static_cast<E*>(a.xhat) + at;
+        for (int k = 0; k < NCH; ++k)
 #pragma unroll
-        for (int k = 0; k < NCH; ++k) store_piece(o, (k * TPR + lane) * 8, p, v[k]);
-    }
-    if (!a.y && !a.q) return;
+            for (int j = 0; j < 8; ++j) v[k][j] *= rstd;
+        if (a.xhat) {
+            E* o = static_cast<E*>(a.xhat) + at;
 #pragma unroll
-    for (int k = 0; k < NCH; ++k) {
-        float(&w)[8] = g[EARLY ? k : 0];
-        if constexpr (!EARLY) load_gamma(a.gamma, a.gamma_bf16, (k * TPR + lane) * 8, p, w);
+            for (int k = 0; k < NCH; ++k) store_piece(o, (k * TPR + lane) * 8, p, v[k]);
+        }
+        if (!a.y) return;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] *= w[j];
-    }
-    if (a.y) {
+        for (int k = 0; k < NCH; ++k) {
+            float w[8];
+            gamma_of(k, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] *= w[j];
+        }
         E* o = static_cast<E*>(a.y) + at;
 #pragma unroll
         for (int k = 0; k < NCH; ++k) store_piece(o, (k * TPR + lane) * 8, p, v[k]);
+        return;
     }
-    if (!a.q) return;
-    // Scales: of the row, or of runs of `group` columns, which are runs of
-    // group / 8 threads within one piece (columns past p hold zeros).  The
-    // quotient y / scale, whose error would move values that lie between two of
-    // the 8-bit ones, is y times the scale's reciprocal, put right by its remainder
-    // (a row whose largest value is infinite has quotients of zero and NaN as they
-    // are).
-    float top = 0.f, m[NCH];
+    // 8-bit rows need h until the end.
+    if (a.xhat) {
+        E* o = static_cast<E*>(a.xhat) + at;
+#pragma unroll
+        for (int k = 0; k < NCH; ++k) {
+            float n[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) n[j] = v[k][j] * rstd;
+            store_piece(o, (k * TPR + lane) * 8, p, n);
+        }
+    }
+    // Threads without columns leave pieces out where a row has many (which also
+    // takes fewer registers: [2000, 16384] in groups of 128 75 us, with them 86).
+    constexpr bool SKIP = NCH * TPR > 1024;
+    Tops m[NCH];
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
-        m[k] = 0.f;
+        const int c = (k * TPR + lane) * 8;
+        m[k] = {0.f, 0.0};
+        if (SKIP && c >= p) continue;
+        float w[8], y[8];
+        gamma_of(k, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m[k] = (k * TPR + lane) * 8 + j < p ? fmaxf(m[k], fabsf(v[k][j])) : m[k];
-        top = fmaxf(top, m[k]);
+        for (int j = 0; j < 8; ++j) y[j] = v[k][j] * rstd * w[j];
+        if (a.y) store_piece(static_cast<E*>(a.y) + at, c, p, y);
+        // (a thread's largest h gamma is that of its largest y, but for magnitudes
+        // that lie within 2^-23 of each other)
+        float h = 0.f, gh = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool take = c + j < p && fabsf(y[j]) > m[k].y;
+            m[k].y = take ? fabsf(y[j]) : m[k].y, h = take ? v[k][j] : h, gh = take ? w[j] : gh;
+        }
+        m[k].t = fabs((double)h * gh);
     }
+    // Scales: of the row, or of runs of `group` columns, which are runs of
+    // group / 8 threads within one piece.  The quotient y / scale is h gamma 448 /
+    // max |h gamma|, for 1 / rms drops out.  It is formed in float64, where h gamma
+    // is exact, and rounded to float32 once: quotients between two 8-bit values
+    // then go to the even one (of bf16 rows with a bf16 gamma about 1 in 10^4
+    // lies there exactly, and float32 sent half of these the other way).  Where
+    // y's largest is zero, next to it or infinite, the quotient is y's own.
+    __shared__ Tops wave[TPR > 64 ? TPR / 64 : 1];
     const int width = a.group ? min(a.group >> 3, TPR) : TPR;
     if (a.group) {
 #pragma unroll
-        for (int k = 0; k < NCH; ++k)
-            for (int off = width >> 1; off >= 1; off >>= 1) m[k] = fmaxf(m[k], __shfl_xor(m[k], off, 64));
+        for (int k = 0; k < NCH; ++k) m[k] = run_tops(m[k], width);
     } else {
-        top = row_reduce<TPR, true>(top, red[1]);
 #pragma unroll
-        for (int k = 0; k < NCH; ++k) m[k] = top;
+        for (int k = 1; k < NCH; ++k) m[0] = larger(m[0], m[k]);
+        m[0] = row_tops<TPR>(m[0], wave);
+#pragma unroll
+        for (int k = 1; k < NCH; ++k) m[k] = m[0];
     }
     uint8_t* q = a.q + at;
     float* qs = a.q_scale + (size_t)row * a.n_groups;
 #pragma unroll
     for (int k = 0; k < NCH; ++k) {
         const int c = (k * TPR + lane) * 8;
-        const float scale = fmaxf(m[k] / 448.0f, 1.17549435e-38f);
-        const float inv = 1.0f / scale;
+        if (SKIP && c >= p) continue;
+        const float exact = m[k].y / 448.0f, scale = fmaxf(exact, 1.17549435e-38f);
+        if (c < p && (a.group ? (lane & (width - 1)) == 0 : lane == 0 && k == 0)) qs[a.group ? c / a.group : 0] = scale;
+        float w[8], u[8];
+        gamma_of(k, w);
+        if constexpr (NCH > 2)
+            // products formed anew: kept, they cost 16 registers a piece
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float t = v[k][j] * inv;
-            v[k][j] = t != 0.f ? fmaf(fmaf(-t, scale, v[k][j]), inv, t) : t;
+            for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(v[k][j]));
+        if (exact > 1.17549435e-38f && exact < INFINITY) {
+            // 448 / max |h gamma|: two Newton steps from an approximation
+            double to = __builtin_amdgcn_rcp(m[k].t);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) to = fma(fma(-m[k].t, to, 1.0), to, to);
+            to *= 448.0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = (float)((double)v[k][j] * w[j] * to);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = v[k][j] * rstd * w[j] / scale;
         }
-        if (c < p) {
-            if (a.group ? (lane & (width - 1)) == 0 : lane == 0 && k == 0) qs[a.group ? c / a.group : 0] = scale;
-            uint32_t w[2];
+        uint32_t b[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(v[k][4 * j], v[k][4 * j + 1], 0, false);
-                w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(v[k][4 * j + 2], v[k][4 * j + 3], w[j], true);
-            }
-            if (c + 8 <= p) {
-                __builtin_memcpy(q + c, w, 8);
-            } else {
+        for (int j = 0; j < 2; ++j) {
+            b[j] = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j], u[4 * j + 1], 0, false);
+            b[j] = __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * j + 2], u[4 * j + 3], b[j], true);
+        }
+        if (c + 8 <= p) {
+            __builtin_memcpy(q + c, b, 8);
+        } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < p) q[c + j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
-            }
+            for (int j = 0; j < 8; ++j)
+                if (c + j < p) q[c + j] = (uint8_t)(b[j >> 2] >> (8 * (j & 3)));
         }
     }
 }
@@ -408,36 +504,48 @@ hipError_t in_launches(int64_t wgs, Go go) {
     return hipSuccess;
 }
 
-template <typename E, int TPR, int NCH>
+template <typename E, bool Q, int TPR, int NCH>
 hipError_t forward(const RmsArgs& a, hipStream_t s) {
     constexpr int rows = block_of<TPR>() / TPR;
     return in_launches((a.rows + rows - 1) / rows, [&](int64_t at, uint32_t n) {
         RmsArgs b = a;
         b.row0 = at * rows;
-        hipLaunchKernelGGL((rmsnorm_kernel<E, TPR, NCH>), dim3(n), dim3(block_of<TPR>()), 0, s, b);
+        hipLaunchKernelGGL((rmsnorm_kernel<E, TPR, NCH, Q>), dim3(n), dim3(block_of<TPR>()), 0, s, b);
     });
+}
+template <typename E, bool Q>
+hipError_t forward(const RmsArgs& a, hipStream_t s) {
+    const int p = a.p;
+    if (p <= 64) return forward<E, Q, 8, 1>(a, s);
+    if (p <= 128) return forward<E, Q, 16, 1>(a, s);
+    if (p <= 256) return forward<E, Q, 32, 1>(a, s);
+    if (p <= 512) return forward<E, Q, 64, 1>(a, s);
+    if (p <= 1024) return forward<E, Q, 64, 2>(a, s);
+    // A piece to a thread: [1024, 1536] 4.9 us, [16384, 2048] 39 (64 threads of
+    // four pieces: 6.4 and 42).
+    if (p <= 2048) return forward<E, Q, 256, 1>(a, s);
+    // Longer rows: a piece to a thread while they are few and a row's latency
+    // counts ([512, 4096] 6.9 us, by 256 threads 7.8); then fewer, busier threads,
+    // with less waiting at the reductions ([2048, 4096] 12.2 us, a piece to a thread
+    // 13.3; with residual and xhat [16384, 5120] 151 us, a piece to a thread 174, by
+    // 256 threads of four pieces 160; in float32 335, 331 and 345).
+    const bool few = a.rows <= 512;
+    if (p <= 4096) return few ? forward<E, Q, 512, 1>(a, s) : forward<E, Q, 256, 2>(a, s);
+    if constexpr (Q) {
+        // 8-bit rows, whose quotients want registers and the vector unit: a piece
+        // to a thread for many rows too (with residual, xhat and groups of 128
+        // [16384, 5120] 192 us, in float32 343; by 256 threads of four pieces 226 and 393).
+        if (p <= 6144) return forward<E, Q, 768, 1>(a, s);
+        if (p <= 8192) return forward<E, Q, 1024, 1>(a, s);
+    } else {
+        if (p <= 8192) return few ? forward<E, Q, 1024, 1>(a, s) : forward<E, Q, 512, 2>(a, s);
+    }
+    if (p <= 16384) return forward<E, Q, 1024, 2>(a, s);
+    return forward<E, Q, 1024, 4>(a, s);
 }
 template <typename E>
 hipError_t forward(const RmsArgs& a, hipStream_t s) {
-    const int p = a.p;
-    if (p <= 64) return forward<E, 8, 1>(a, s);
-    if (p <= 128) return forward<E, 16, 1>(a, s);
-    if (p <= 256) return forward<E, 32, 1>(a, s);
-    if (p <= 512) return forward<E, 64, 1>(a, s);
-    if (p <= 1024) return forward<E, 64, 2>(a, s);
-    // A piece to a thread: [1024, 1536] 4.9 us, [16384, 2048] 39 (64 threads of
-    // four pieces: 6.4 and 42).
-    if (p <= 2048) return forward<E, 256, 1>(a, s);
-    // Longer rows: a piece to a thread while they are few and a row's latency
-    // counts ([48, 5120] with e4m3 4.8 us, by 256 threads 8.1; [512, 4096] 6.9
-    // and 7.8); then fewer, busier threads, with less waiting at the reductions
-    // ([2048, 4096] 12.2 us, a piece to a thread 13.3; [16384, 5120] 131 and 137,
-    // with e4m3 154 and 175).
-    const bool few = a.rows <= 512;
-    if (p <= 4096) return few ? forward<E, 512, 1>(a, s) : forward<E, 256, 2>(a, s);
-    if (p <= 8192) return few ? forward<E, 1024, 1>(a, s) : forward<E, 256, 4>(a, s);
-    if (p <= 16384) return forward<E, 1024, 2>(a, s);
-    return forward<E, 1024, 4>(a, s);
+    return a.q ? forward<E, true>(a, s) : forward<E, false>(a, s);
 }
 
 template <typename E, int TPR, int NCH, int BLOCK = block_of<TPR>()>
