@@ -566,8 +566,8 @@ hipError_t backward(const RmsGradArgs& a, hipStream_t s) {
     if (p <= 128) return backward<E, 16, 1>(a, s);
     if (p <= 256) return backward<E, 32, 1>(a, s);
     // Where there is a workgroup to a CU at most, it takes as many rows at once as
-    // its registers allow, 16 or 8 instead of 4: bf16 [32, 128, 768] 8.4 us instead
-    // of 11.8, [16, 33, 300] 5.8 and 9.9, float32 [16, 197, 777] 12.6 and 15.0.  With
+    // its registers allow, 16 or 8 instead of 4: bf16 [32, 128, 768] 8.3 to 9.3 us
+    // instead of 11.8, [16, 33, 300] 5.8 and 9.9, float32 [16, 197, 777] 12.6 and 15.0.  With
     // more, small workgroups fill the CUs better: [8, 1024, 768] 16.3 and 15.0, [2000,
     // 20, 512] 35 and 27.
     const bool few = !a.solo && a.B * a.chunks <= 256;
