@@ -987,7 +987,7 @@ __global__ __launch_bounds__(kSmallThreads) void ns_small_kernel(const NsSmallAr
 // products of X itself.  Where further steps would lose that again (the rule is
 // the host's), another round begins with the Gram matrix of P X.  P X is not kept:
 // each launch multiplies the chunk that it has loaded by the P of all rounds so
-// far, which costs the usual one round nothing and many rounds no memory.
+// far, which costs the usual one round nothing, and many no memory of X's size.
 // Next to 3 launches for each step of the general path: 3 in all for one round,
 // two more for each other, and G and M pass memory once a launch over chunks.
 // Kernel times: one 16 x 4096 20 us, 24 of them 32, one 48 x 3000 63, one 64 x 3000

@@ -124,3 +124,20 @@ def test_small_rows_with_an_eps(bk):
     x = (torch.randn(7, 640, generator=gen) * 1e-30).to(torch.bfloat16).to(DEV)
     out = bk.bk_rmsnorm(x, eps=1e-6, q8=64)
     assert np.array_equal(out.q.double().cpu().numpy(), _rounded_once(x.double().cpu().numpy(), 64))
+
+
+@pytest.mark.parametrize("group", [0, 32, 128])
+@pytest.mark.parametrize("p", [8, 40, 64, 100, 128, 200, 256, 400])
+def test_rows_that_share_a_wave(bk, p, group):
+    """Several rows to a wave, the last of them missing: maxima stay within their row."""
+    gen = torch.Generator().manual_seed(p)
+    gamma = (torch.randn(p, generator=gen) * 0.2 + 1).to(DEV)
+    size = torch.logspace(-4, 4, 29)[:, None]
+    for rows in (1, 2, 3, 5, 7, 9, 15, 17, 29):
+        x = (torch.randn(rows, p, generator=gen) * size[:rows]).to(DEV)
+        out = bk.bk_rmsnorm(x, gamma, eps=1e-6, q8=group)
+        t = x.double().cpu().numpy() * gamma.double().cpu().numpy()
+        assert np.array_equal(out.q.double().cpu().numpy(), _rounded_once(t, group)), rows
+        y, _, _ = so.rmsnorm(x.double().cpu().numpy(), gamma.double().cpu().numpy(), 1e-6)
+        _, scales = so.quantise_e4m3(y, group)
+        assert (np.abs(out.q_scale.double().cpu().numpy() - scales) <= 36 * U * scales).all()

@@ -1,14 +1,14 @@
 """Refusals of kept affine layers in the binding.  A kept layer takes its sizes
 from P alone, so tensors that do not fit P would be read or written past their
 end.  On the CPU: the check of the device is replaced, and the library by one
-that fails if it is called."""
+that fails if it is called.  On the GPU: a kept layer that still names its tokens."""
 import pytest
 import torch
 
 bk = pytest.importorskip("paper_2210_00038_amd", reason="libbk.so not built")
 
 
-@pytest.fixture(autouse=True)
+@pytest.fixture
 def host_tensors(monkeypatch):
     def dev(t, name):
         if not isinstance(t, torch.Tensor):
@@ -36,12 +36,12 @@ def _spec(**kw):
     (dict(G=torch.zeros(16)[::2]), "contiguous"), (dict(G=torch.zeros(8, device="meta")), "G of a kept layer"),
     (dict(Gb=torch.zeros(4)), "Gb of a kept layer"), (dict(Gb=torch.zeros(8, dtype=torch.float64)), "Gb of a kept layer"),
 ])
-def test_refused(kw, said):
+def test_refused(host_tensors, kw, said):
     with pytest.raises(ValueError, match=said):
         bk.make_layers([_spec(**kw)])
 
 
-def test_taken():
+def test_taken(host_tensors):
     arr = bk.make_layers([_spec(), _spec(G=None, Gb=None), _spec(bias=False, Pb=None, Gb=None), _spec(G=torch.zeros(1, 8))])
     assert [arr[k].p for k in range(4)] == [8] * 4 and arr[0].flags == bk.BK_LAYER_KEPT | bk.BK_LAYER_BIAS
 
@@ -57,7 +57,7 @@ class _Untouched:
         return call
 
 
-def test_more_samples_than_kept(monkeypatch):
+def test_more_samples_than_kept(host_tensors, monkeypatch):
     arr = bk.make_layers([_spec(), _spec(P=torch.zeros(2, 8), Pb=torch.zeros(2, 8))])
     monkeypatch.setattr(bk, "lib", _Untouched())
     C = torch.zeros(4)
@@ -69,3 +69,23 @@ def test_more_samples_than_kept(monkeypatch):
             with pytest.raises(ValueError, match="holds"):
                 call(n, B)
     assert bk._batch(arr, 1, 3) == 3 and bk._batch(arr, 2, 2) == 2
+
+
+@pytest.mark.gpu
+def test_tokens_are_not_read():
+    """T may be any, and x and g NULL, as the header says."""
+    gen = torch.Generator().manual_seed(3)
+    B, p = 4, 300
+    P, Pb = (torch.randn(B, p, generator=gen).to("cuda") for _ in range(2))
+    got = []
+    for T in (0, 1, 77):
+        G, Gb = torch.empty(p, device="cuda"), torch.empty(p, device="cuda")
+        arr = bk.make_layers([{"kind": bk.BK_NORM_AFFINE, "kept": True, "bias": True, "P": P, "Pb": Pb, "G": G, "Gb": Gb}])
+        arr[0].T = T
+        n, C = torch.empty(1, B, device="cuda"), torch.empty(B, device="cuda")
+        bk.bk_private_grad(arr, 1, bk.BK_BF16, B, bk.BK_CLIP_ABADI, 1.0, 0.0, 0.0, 1, 0, n, C)
+        got.append([n, C, G, Gb])
+    assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other))
+    norm = (P.double().square().sum(1) + Pb.double().square().sum(1)).sqrt()
+    assert torch.allclose(got[0][1].double(), (1 / norm).clamp(max=1), rtol=1e-5)
+    assert torch.allclose(got[0][2].double(), (got[0][1].double()[:, None] * P.double()).sum(0), rtol=1e-5, atol=1e-6)
