@@ -249,6 +249,10 @@ def _workspace(nbytes: int, device, ws: Optional[torch.Tensor]):
         return None, 0
     if ws is None:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    else:
+        _dev(ws, "the workspace")
+        if isinstance(device, torch.device) and device.index not in (None, ws.get_device()):
+            raise ValueError(f"the workspace must be on {device}, not on {ws.device}")
     return ws, ws.numel() * ws.element_size()
 
 
