@@ -223,3 +223,18 @@ def test_muon_step_of_many_steps(bk):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y)), rep
+
+
+@pytest.mark.parametrize("d,p", [(16, 768), (16, 4096), (1, 5000), (900, 33), (100, 201)])
+def test_zero_nan_and_infinity(bk, d, p):
+    """After many steps too a zero update stays zero, and a NaN or an infinity spoils its whole matrix and no other."""
+    U = _update("full", d, p)
+    for steps in (1, 20, 64):
+        for poison in (float("nan"), float("inf"), float("-inf")):
+            G = [torch.tensor(U).to(DEV) for _ in range(4)]
+            G[1].zero_()
+            G[2][d - 1, p // 2] = poison
+            O = [torch.empty(d, p, device=DEV) for _ in G]
+            bk.bk_orthogonalize(bk.make_matrices([{"G": g, "O": o} for g, o in zip(G, O)]), 4, bk.BK_NS_F32, steps=steps)
+            assert (O[1] == 0).all() and O[2].isnan().all(), (steps, poison)
+            assert O[0].isfinite().all() and torch.equal(O[0], O[3])
